@@ -232,6 +232,7 @@ __global__ void __launch_bounds__(Threads, kCtas) distill_kernel(DistillArgs a) 
   const int ctas = static_cast<int>(cluster.num_blocks());
   const int rank = static_cast<int>(cluster.block_rank());
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (ctas > 1) cluster.barrier_arrive(); // (this CTA has begun: its peers may write to parts)
   const float c = kLog2e / a.temperature;
   const Two c2 = two(c, c);
   const int64_t row = blockIdx.x / static_cast<unsigned>(ctas);
@@ -340,6 +341,7 @@ __global__ void __launch_bounds__(Threads, kCtas) distill_kernel(DistillArgs a) 
   x = warp_join(lane < kWarps ? warps[lane] : MaxSum{Values<T>::kLowest, 0.f}, c);
   y = warp_join(lane < kWarps ? teachers[lane] : MaxSum{Values<float>::kLowest, 0.f}, c);
   if (ctas > 1) {
+    cluster.barrier_wait();               // long past: all CTAs of the cluster have begun
     if (warp == 0 && lane < ctas) *cluster.map_shared_rank(&parts[rank], lane) = x;
     cluster.sync();
     x = warp_join(lane < ctas ? parts[lane] : MaxSum{Values<T>::kLowest, 0.f}, c);
