@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(Threads, kCtas) distill_kernel(DistillArgs a) 
   extern __shared__ __align__(16) uint4 ring[];
   __shared__ int ids[E * Threads];        // of the results that take part, else -1
   __shared__ float shares[E * Threads];
-  __shared__ unsigned short met[kPlaces]; // by hashing: a result that has the id, or kNone
+  // By hashing: a result that has the id, or kNone (cleared as words).
+  __shared__ __align__(16) unsigned short met[kPlaces];
   __shared__ MaxSum warps[kWarps], teachers[kWarps], parts[kMaxCluster];
   __shared__ float terms[kWarps];
   __shared__ int repeated;                // an id that two results have

@@ -100,7 +100,8 @@ scatter_kernel(SortArgs a, const uint2* in, uint2* out, int pass) {
   constexpr int kWarps = Threads / 32;
   constexpr int kTile = kItems * Threads;
   constexpr int kOwn = Threads < kMaxDigits ? kMaxDigits / Threads : 1;   // digits of a thread, at most
-  __shared__ uint16_t hist[kWarps][kMaxDigits];   // counts per warp, then tokens before
+  // Counts per warp, then tokens before (cleared as words).
+  __shared__ __align__(16) uint16_t hist[kWarps][kMaxDigits];
   __shared__ uint32_t base[kMaxDigits], sums[kWarps];
   __shared__ uint4 part[2][Threads];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

@@ -28,3 +28,12 @@ def test_a_peers_shared_memory_is_touched_behind_a_cluster_barrier(name):
         first = kernel.find("map_shared_rank(")
         if first >= 0:
             assert re.search(r"cluster\.(sync|barrier_wait)\(", kernel[:first]), name
+
+
+@pytest.mark.parametrize("name", SOURCES)
+def test_shared_arrays_of_small_values_state_their_alignment(name):
+    """An array of 1- or 2-byte values lies on any such boundary unless it says
+    otherwise, and the kernels clear and copy such arrays in words."""
+    small = r"(u?int(8|16)_t|(unsigned\s+|signed\s+)?(short|char)|__half|__nv_bfloat16)"
+    found = re.findall(rf"__shared__\s+{small}\s+\w+\s*\[", _code(name))
+    assert not found, name
