@@ -472,7 +472,9 @@ OPRAG_API int oprag_embed_pool_train(const void *hidden, int32_t hidden_dtype, i
  * Gradient of the embedding tail: with y = m / ||m|| and grad = dloss/dy,
  *   dloss/dhidden[b][t] = (grad[b] - y (y . grad[b])) / (||m|| c)
  * for a real token t of the c of text b, 0 for padding and for a text with
- * c = 0 or m = 0.
+ * c = 0 or m = 0.  Finite means of any size have this gradient (oprag_embed_pool's
+ * rows are zero where ||m||^2 leaves the range of fp32: ||m|| above 1.8e19, or
+ * every value below 2e-23); one that is infinite or not a number has NaN.
  *   grad        device, batch x dim, 16-byte aligned.
  *   mean        device, batch x dim floats of oprag_embed_pool_train.
  *   mask        as given to oprag_embed_pool_train.

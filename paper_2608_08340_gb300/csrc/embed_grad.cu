@@ -1,12 +1,15 @@
 // Gradient of the embedding tail y = m / |m|, m = the mean of a text's real hidden
 // states: dm = (g - y (y . g)) / |m| for the gradient g of y, and dm / c for each of
 // the text's c real tokens, 0 for its padding.  A text without real tokens, or with
-// m = 0, has no gradient.
+// m = 0, has no gradient; a mean that is infinite or not a number has one that is not a
+// number.
 //
 // Bound by HBM writes: batch x tokens x dim values from two rows per text.  A CTA forms
 // the text's row in shared memory, rounded, and copies it to a chunk of its tokens; the
 // sums over the row are formed again by every chunk's CTA (its rows come from L2).
 // 256 x 512 x 4096 bf16: 156 us, 6.9 TB/s; values formed again per token took 258.
+#include <cmath>
+
 #include "internal.h"
 #include "values.cuh"
 
@@ -17,6 +20,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxDim = 16384;
+// Squared norms between which neither the squares nor the products with a gradient lose
+// what counts: a value whose square is lost is below 2^-54 of the norm.
+constexpr float kLeast = 0x1p-40f, kMost = 0x1p40f;
 
 template <typename T>
 __device__ __forceinline__ void load4(const T* src, float (&v)[4]) {
@@ -43,46 +49,75 @@ embed_pool_grad_kernel(const TIn* __restrict__ grad, const float* __restrict__ m
   extern __shared__ __align__(16) unsigned char shared[];
   TOut* row = reinterpret_cast<TOut*>(shared);
   __shared__ float sums[3][kWarps];
+  __shared__ uint32_t tops[kWarps];
   const int64_t b = blockIdx.x;
   const float* m = mean + b * dim;
   const TIn* g = grad + b * dim;
   const uint8_t* mrow = mask + b * tokens;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float part[3] = {0.f, 0.f, 0.f};                // m . m, m . g, real tokens
+  // (m / 2^e) . (m / 2^e), (m / 2^e) . g and the real tokens.
+  float part[3];
+  auto add_up = [&](int e) {
+    part[0] = part[1] = part[2] = 0.f;
+    for (int i = 4 * threadIdx.x; i < dim; i += 4 * kThreads) {
+      float x[4], y[4];
+      load4(m + i, x);
+      load4(g + i, y);
+#pragma unroll
+      for (int l = 0; l < 4; ++l) {
+        if (e != 0) x[l] = scalbnf(x[l], -e);
+        part[0] = fmaf(x[l], x[l], part[0]);
+        part[1] = fmaf(x[l], y[l], part[1]);
+      }
+    }
+    for (int t = threadIdx.x; t < tokens; t += kThreads) part[2] += mrow[t] != 0 ? 1.f : 0.f;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) part[k] += __shfl_xor_sync(0xffffffffu, part[k], o);
+      if (lane == 0) sums[k][warp] = part[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      part[k] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) part[k] += sums[k][w];
+    }
+  };
+  add_up(0);
+  // A mean whose squares may leave the range is taken as 2^e (m / 2^e), its largest
+  // magnitude being in [2^e, 2^(e + 1)): no rounding, so the same bits as without.
+  int e = 0;
+  if (part[2] > 0.f && !(part[0] >= kLeast && part[0] <= kMost)) {
+    uint32_t top = 0;                             // (ordered as the magnitudes are)
+    for (int i = threadIdx.x; i < dim; i += kThreads) top = max(top, __float_as_uint(fabsf(m[i])));
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();                              // (the sums are read)
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = max(top, tops[w]);
+    if (top >= __float_as_uint(INFINITY)) {       // infinite, or not a number: no direction
+      part[0] = NAN;
+    } else if (top != 0) {
+      e = ilogbf(__uint_as_float(top));
+      add_up(e);
+    }
+  }
+  const float mm = part[0], mg = part[1], real = part[2];
+  const bool there = real > 0.f && mm != 0.f;     // (what is not a number is passed on)
+  const float by = there ? 1.f / (real * sqrtf(mm)) : 0.f;
+  const float along = there ? mg / mm : 0.f;      // (y . g) / (|m| / 2^e)
   for (int i = 4 * threadIdx.x; i < dim; i += 4 * kThreads) {
     float x[4], y[4];
     load4(m + i, x);
     load4(g + i, y);
 #pragma unroll
     for (int l = 0; l < 4; ++l) {
-      part[0] = fmaf(x[l], x[l], part[0]);
-      part[1] = fmaf(x[l], y[l], part[1]);
+      if (e != 0) x[l] = scalbnf(x[l], -e);
+      y[l] = there ? (y[l] - x[l] * along) * by : 0.f;
+      if (e != 0) y[l] = scalbnf(y[l], -e);
     }
-  }
-  for (int t = threadIdx.x; t < tokens; t += kThreads) part[2] += mrow[t] != 0 ? 1.f : 0.f;
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) part[k] += __shfl_xor_sync(0xffffffffu, part[k], o);
-    if (lane == 0) sums[k][warp] = part[k];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    part[k] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) part[k] += sums[k][w];
-  }
-  const float mm = part[0], mg = part[1], real = part[2];
-  // (a mean that is not a number has a gradient that is none either)
-  const float by = real > 0.f && mm != 0.f ? 1.f / (real * sqrtf(mm)) : 0.f;
-  const float along = by != 0.f ? mg / mm : 0.f;  // (y . g) / |m|
-  for (int i = 4 * threadIdx.x; i < dim; i += 4 * kThreads) {
-    float x[4], y[4];
-    load4(m + i, x);
-    load4(g + i, y);
-#pragma unroll
-    for (int l = 0; l < 4; ++l) y[l] = by != 0.f ? (y[l] - x[l] * along) * by : 0.f;
     store_values(row + i, y);
   }
   __syncthreads();

@@ -1,13 +1,15 @@
 """GPU parity of the training operators on the plans that large calls take: rows that
 clusters of every size share, sorts of many tiles, several column slabs, long rows.
 References and error bounds are those of test_gpu_train.py."""
+import math
 
 import pytest
 import torch
 
-from paper_2608_08340_gb300.train import distill_loss
+from paper_2608_08340_gb300.train import distill_loss, embed_pool_grad
 
-from test_gpu_train import _distill_plain, _rand, _teacher, _within
+from test_gpu_train import (DT, _distill_plain, _pool_grad_plain, _rand, _tail_mask, _teacher,
+                            _within)
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +35,33 @@ def test_distill_of_many_rows_that_clusters_share(dtype, kb, q):
                                                             0.1, None)
         _within(loss[part].cpu(), want, loss_bound, "f32", f"loss {i}")
         _within(dz[part].cpu(), grad, grad_bound, dtype, f"gradient {i}")
+
+
+# ------------------------------------------------------- the embedding tail
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("d", [8, 392, 4104])
+@pytest.mark.parametrize("size,by", [(1e25, 1.0), (2e37, 1.0), (1e-25, 1.0), (1e-36, 1e-3),
+                                     (1e-41, 1e-9)])
+def test_pool_grad_of_means_whose_squares_leave_the_range(dtype, out, d, size, by):
+    """Finite means of any size have the definition's gradient."""
+    mask = _tail_mask(6, 9, d)
+    mean, grad = _rand((6, d), "f32", d, 1.0), _rand((6, d), dtype, d + 1, by)
+    mean[0] *= size
+    mean[3] *= size
+    mean[4] *= size
+    mean[4, 1:] = 0                               # one value alone
+    mean[5, ::2] *= size                          # large and small ones
+    row, bound = _pool_grad_plain(grad, mean, mask)
+    _within(embed_pool_grad(grad, mean, mask, DT[out], per_token=False).cpu(), row, bound, out)
+
+
+def test_pool_grad_of_an_infinite_mean_is_not_a_number():
+    mask = torch.ones(4, 6, dtype=torch.bool, device="cuda")
+    mask[:, 4:] = False
+    mean, grad = _rand((4, 64), "f32", 1), _rand((4, 64), "f32", 2)
+    clean = embed_pool_grad(grad, mean, mask, torch.float32)
+    mean[1, 3], mean[2, 5] = math.inf, -math.inf
+    got = embed_pool_grad(grad, mean, mask, torch.float32)
+    assert got[1:3, :4].isnan().all() and (got[1:3, 4:] == 0).all()
+    assert torch.equal(got[[0, 3]], clean[[0, 3]])
