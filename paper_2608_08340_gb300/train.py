@@ -12,8 +12,9 @@ the scores are held to the results.  One training step:
 
 Every call enqueues hand-written kernels of liboprag.so on `stream` (a
 torch.cuda.Stream; default: the current one) and returns tensors that belong to that
-stream.  Inputs have to be ready on it.  Rows that are not laid out as a kernel reads
-them are copied on that stream first.
+stream.  Inputs have to be ready on it; they may be dropped behind the call, their memory
+is not given away before that stream has got past it.  Rows that are not laid out as a
+kernel reads them are copied on that stream first.
 """
 from __future__ import annotations
 
@@ -60,6 +61,17 @@ def _call(name: str, *args) -> None:
         check(rc)
 
 
+def _on(stream, call, *args):
+    """call(*args) with `stream` current; its tensors, which may be another stream's, are
+    kept for it."""
+    with torch.cuda.stream(stream):
+        result = call(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    return result
+
+
 def _check_sizes(*sizes: int) -> None:
     """The C ABI takes these sizes in 32 bits, and ctypes would cut them off."""
     if max(sizes) > 0x7FFFFFFF:
@@ -101,8 +113,7 @@ def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     of any shape, an id outside [0, vocab) gives a zero row (padding).  Returns
     ids.shape + (dim,)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return embed_lookup(table, ids, scale, out_dtype, None, out)
+        return _on(stream, embed_lookup, table, ids, scale, out_dtype, None, out)
     rows = table.shape
     if len(rows) != 2 or table.dtype not in _DT:
         raise ValueError("table must be a 2-D bfloat16 or float32 tensor")
@@ -143,8 +154,7 @@ def embed_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: 
     rows.unsqueeze(1).expand(-1, tokens, -1) where all tokens of a text share a row:
     it is read as it lies.  ids as for embed_lookup, with at least one dimension."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return embed_lookup_grad(grad, ids, vocab, scale, out_dtype, None, out)
+        return _on(stream, embed_lookup_grad, grad, ids, vocab, scale, out_dtype, None, out)
     if grad.dtype not in _DT or ids.dtype not in _IDS:
         raise ValueError("grad must be bfloat16 or float32, ids int32 or int64")
     if ids.dim() < 1 or grad.dim() != ids.dim() + 1 or grad.shape[:-1] != ids.shape:
@@ -187,8 +197,7 @@ def embed_pool_train(hidden: torch.Tensor, mask: torch.Tensor,
     """embed_pool that keeps what its gradient needs: (out, mean), mean the float32
     (batch, dim) pooled rows before normalisation."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return embed_pool_train(hidden, mask, out_dtype)
+        return _on(stream, embed_pool_train, hidden, mask, out_dtype)
     if hidden.dim() != 3 or hidden.dtype not in _DT:
         raise ValueError("hidden must be a 3-D bfloat16 or float32 tensor")
     if out_dtype not in _DT:
@@ -218,8 +227,7 @@ def embed_pool_grad(grad: torch.Tensor, mean: torch.Tensor, mask: torch.Tensor,
     grad: (batch, dim) gradient of embed_pool_train's out; mean: its second result;
     mask: the mask that it was given."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return embed_pool_grad(grad, mean, mask, dtype, per_token)
+        return _on(stream, embed_pool_grad, grad, mean, mask, dtype, per_token)
     if grad.dim() != 2 or grad.dtype not in _DT:
         raise ValueError("grad must be a 2-D bfloat16 or float32 tensor")
     if mean.shape != grad.shape or mean.dtype != torch.float32:
@@ -259,9 +267,8 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
     and no gradient.  grad=False: (loss, None).  out: where the gradient goes, a (q, n)
     tensor with contiguous rows; it may be logits."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return distill_loss(logits, teacher_ids, teacher_scores, temperature, weight, grad,
-                                None, out)
+        return _on(stream, distill_loss, logits, teacher_ids, teacher_scores, temperature, weight,
+                   grad, None, out)
     shape, results = logits.shape, teacher_ids.shape
     if len(shape) != 2 or logits.dtype not in _DT:
         raise ValueError("logits must be a 2-D bfloat16 or float32 tensor")

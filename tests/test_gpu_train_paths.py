@@ -6,7 +6,8 @@ import math
 import pytest
 import torch
 
-from paper_2608_08340_gb300.train import distill_loss, embed_pool_grad
+from paper_2608_08340_gb300.train import (distill_loss, embed_lookup, embed_lookup_grad,
+                                          embed_pool_grad, embed_pool_train)
 
 from test_gpu_train import (DT, _distill_plain, _pool_grad_plain, _rand, _tail_mask, _teacher,
                             _within)
@@ -65,3 +66,44 @@ def test_pool_grad_of_an_infinite_mean_is_not_a_number():
     got = embed_pool_grad(grad, mean, mask, torch.float32)
     assert got[1:3, :4].isnan().all() and (got[1:3, 4:] == 0).all()
     assert torch.equal(got[[0, 3]], clean[[0, 3]])
+
+
+# ------------------------------------------------------------------ streams
+
+def _calls():
+    """(call of a stream and an output or None, its inputs) for every operator."""
+    table, ids = _rand((3000, 512), "f32", 1), torch.randint(0, 3000, (64, 90), device="cuda")
+    hidden, mask = _rand((64, 90, 512), "f32", 2), torch.ones(64, 90, dtype=torch.bool, device="cuda")
+    mean, grad = _rand((64, 512), "f32", 3), _rand((64, 512), "f32", 4)
+    logits, weight = _rand((64, 5000), "f32", 5), torch.rand(64, device="cuda")
+    t_ids, t_scores = _teacher(64, 5000, 9, 6)
+    return {
+        "lookup": (lambda a, s: embed_lookup(*a, stream=s), [table, ids]),
+        "lookup_grad": (lambda a, s: embed_lookup_grad(*a, 3000, stream=s), [hidden, ids]),
+        "pool_train": (lambda a, s: embed_pool_train(*a, stream=s), [hidden, mask]),
+        "pool_grad": (lambda a, s: embed_pool_grad(*a, stream=s), [grad, mean, mask]),
+        "distill": (lambda a, s: distill_loss(*a[:3], 0.3, a[3], stream=s),
+                    [logits, t_ids, t_scores, weight]),
+    }
+
+
+@pytest.mark.parametrize("name", ["lookup", "lookup_grad", "pool_train", "pool_grad", "distill"])
+def test_inputs_may_be_dropped_behind_a_call_on_another_stream(name):
+    """The memory of a dropped input is not given away while the stream that the call
+    was given still has to read it."""
+    call, inputs = _calls()[name]
+    want = call(inputs, None)
+    s = torch.cuda.Stream()
+    mine = [t.clone() for t in inputs]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)            # cycles: about a tenth of a second
+    got = call(mine, s)
+    del mine
+    others = [torch.zeros_like(t) for t in inputs for _ in range(3)]     # on the current stream
+    torch.cuda.current_stream().synchronize()
+    s.synchronize()
+    for a, b in zip(want if isinstance(want, tuple) else [want],
+                    got if isinstance(got, tuple) else [got]):
+        assert torch.equal(a, b)
+    del others
