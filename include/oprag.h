@@ -422,7 +422,8 @@ OPRAG_API int oprag_search_noalloc(oprag_index *idx, const void *queries, int32_
  * larger encoder's searches ranked them.  The calls below are the steps that
  * are no plain matrix product.  They need no index, run on the current device,
  * enqueue on `stream` and keep nothing between calls; a gradient is rounded to
- * its dtype once, from fp32.
+ * its dtype once, from fp32.  An output that lies over the table, the gradient or
+ * the scores that the call reads is refused (but see oprag_distill).
  *
  * Embedding lookup: out[i] = scale * table[ids[i]], a zero row for an id
  * outside [0, vocab) (padding).
@@ -508,7 +509,8 @@ OPRAG_API int oprag_embed_pool_grad(const void *grad, int32_t grad_dtype, const 
  *   weight      device, q floats, or NULL for 1.
  *   loss        device, q floats (not weighted).
  *   grad        device, q rows in the logits' dtype, grad_stride values apart;
- *               may be logits itself with the same stride.  NULL: loss only.
+ *               may be logits itself with the same stride, or lie apart from
+ *               its rows (between them, say).  NULL: loss only.
  */
 OPRAG_API int oprag_distill(const void *logits, int32_t dtype, int64_t row_stride, int32_t q,
                             int32_t n, const int64_t *teacher_ids, const float *teacher_scores,

@@ -5,6 +5,7 @@
 
 #include "oprag.h"
 #include "internal.h"
+#include "overlap.h"
 
 using namespace oprag;
 
@@ -14,6 +15,27 @@ bool is_dtype(int32_t d) { return d == OPRAG_F32 || d == OPRAG_BF16; }
 int dtype_of(int32_t d) { return d == OPRAG_BF16 ? kBF16 : kF32; }
 int64_t size_of(int32_t d) { return d == OPRAG_BF16 ? 2 : 4; }
 bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+Rows rows_of(const void* at, int64_t rows, int64_t bytes, int64_t stride) {
+  return {reinterpret_cast<uintptr_t>(at), rows, bytes, stride};
+}
+
+// Whether out, `bytes` long, lies over a gradient of texts x tokens rows (strides in bytes,
+// any of them 0).
+bool over_gradient(const void* out, int64_t bytes, const void* grad, int64_t texts, int64_t tokens,
+                   int64_t row, int64_t text_stride, int64_t token_stride) {
+  if (texts < 1 || tokens < 1) return false;
+  const Rows to = rows_of(out, 1, bytes, bytes);
+  // A text's rows, one block where they touch.
+  const int64_t text = (tokens - 1) * token_stride + row;
+  Rows part = token_stride > row ? rows_of(grad, tokens, row, token_stride)
+                                 : rows_of(grad, 1, text, text);
+  const int64_t whole = (texts - 1) * text_stride + text;
+  if (!overlap(to, rows_of(grad, 1, whole, whole))) return false;
+  for (int64_t b = 0; b < (text_stride == 0 ? 1 : texts); ++b, part.at += text_stride)
+    if (overlap(to, part)) return true;
+  return false;
+}
 
 }  // namespace
 
@@ -37,6 +59,9 @@ int oprag_embed_lookup(const void* table, int32_t table_dtype, int64_t vocab, in
   if (!table || !ids || !out) return fail(OPRAG_ERR_INVALID_ARG, "NULL argument");
   if (!aligned(table) || !aligned(out))
     return fail(OPRAG_ERR_INVALID_ARG, "table and out must be 16-byte aligned");
+  const int64_t size = size_of(table_dtype), bytes = count * dim * size_of(out_dtype);
+  if (overlap(rows_of(out, 1, bytes, bytes), rows_of(table, vocab, dim * size, row_stride * size)))
+    return fail(OPRAG_ERR_INVALID_ARG, "out overlaps table");
   const LookupArgs a{table, dtype_of(table_dtype), vocab, row_stride, dim, ids, ids_64 != 0, count,
                      scale, out, dtype_of(out_dtype)};
   const cudaError_t e = launch_embed_lookup(a, static_cast<cudaStream_t>(stream));
@@ -78,6 +103,9 @@ int oprag_embed_lookup_grad(const void* grad, int32_t grad_dtype, int64_t texts,
   if (workspace_bytes < need)
     return fail(OPRAG_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed",
                 static_cast<long long>(workspace_bytes), static_cast<long long>(need));
+  if (over_gradient(out, vocab * dim * size_of(out_dtype), grad, texts, tokens, dim * size,
+                    text_stride * size, token_stride * size))
+    return fail(OPRAG_ERR_INVALID_ARG, "out overlaps grad");
   const LookupGradArgs a{grad, dtype_of(grad_dtype), count, tokens, text_stride, token_stride, dim,
                          ids, ids_64 != 0, vocab, scale, out, dtype_of(out_dtype), workspace};
   const cudaError_t e = launch_embed_lookup_grad(a, static_cast<cudaStream_t>(stream));
@@ -139,6 +167,12 @@ int oprag_distill(const void* logits, int32_t dtype, int64_t row_stride, int32_t
   const uintptr_t bits = reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad);
   if (bits % size_of(dtype) != 0)
     return fail(OPRAG_ERR_INVALID_ARG, "logits and grad must be aligned to their values");
+  const int64_t size = size_of(dtype);
+  if (grad && !(grad == logits && (q == 1 || grad_stride == row_stride)) &&
+      overlap(rows_of(logits, q, n * size, row_stride * size),
+              rows_of(grad, q, n * size, grad_stride * size)))
+    return fail(OPRAG_ERR_INVALID_ARG,
+                "grad overlaps logits: it may be logits itself, with its stride, or lie apart");
   const DistillArgs a{logits, dtype_of(dtype), row_stride, q, n, k, teacher_ids, teacher_scores,
                       temperature, weight, loss, grad, grad_stride};
   const cudaError_t e = launch_distill(a, static_cast<cudaStream_t>(stream));

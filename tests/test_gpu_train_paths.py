@@ -107,3 +107,31 @@ def test_inputs_may_be_dropped_behind_a_call_on_another_stream(name):
                     got if isinstance(got, tuple) else [got]):
         assert torch.equal(a, b)
     del others
+
+
+# ------------------------------------------------- outputs beside the inputs
+
+def test_outputs_between_the_rows_of_the_inputs():
+    """Rows that lie between the other's rows are apart from them; over them, refused."""
+    both = _rand((40, 2048), "f32", 1)
+    logits, other = both[:, :1000], both[:, 1000:2000]
+    ids, scores = _teacher(40, 1000, 9, 2)
+    want_loss, want = distill_loss(logits.clone(), ids, scores, 0.3)
+    loss, dz = distill_loss(logits, ids, scores, 0.3, out=other)
+    assert dz is other and torch.equal(dz, want) and torch.equal(loss, want_loss)
+    for out in (both[:, 999:1999], both[:, 1:1001], both.view(-1)[:40 * 1000].view(40, 1000)):
+        with pytest.raises(RuntimeError, match="overlap"):
+            distill_loss(logits, ids, scores, 0.3, out=out)
+    wide = _rand((50, 96), "f32", 3)
+    rows = torch.tensor([3, 49, 0], device="cuda")
+    want = embed_lookup(wide[:, :32], rows, 2.0)
+    out = wide[7, 32:].view(2, 32)                # in a gap of the table
+    assert torch.equal(embed_lookup(wide[:, :32], rows[:2], 2.0, out=out), want[:2])
+    with pytest.raises(RuntimeError, match="overlap"):
+        embed_lookup(wide[:, :32], rows, 2.0, out=wide[7].view(3, 32))
+    grad = _rand((6, 5, 32), "f32", 4)
+    ids = torch.randint(0, 10, (6, 5), device="cuda")
+    want = embed_lookup_grad(grad[2:].clone(), ids[2:], 10)
+    assert torch.equal(embed_lookup_grad(grad[2:], ids[2:], 10, out=grad[:2].view(10, 32)), want)
+    with pytest.raises(RuntimeError, match="overlap"):
+        embed_lookup_grad(grad[1:], ids[1:], 10, out=grad[:2].view(10, 32))
