@@ -15,12 +15,19 @@ torch.cuda.Stream; default: the current one) and returns tensors that belong to 
 stream.  Inputs have to be ready on it; they may be dropped behind the call, their memory
 is not given away before that stream has got past it.  Rows that are not laid out as a
 kernel reads them are copied on that stream first.
+
+Under torch's automatic differentiation embed_lookup's rows, embed_pool_train's out and
+distill_loss's loss lead back to a table, hidden states and logits that require a
+gradient, through the calls above (so `loss.mean().backward()` does the rest of the
+step); the teacher's results, the weight and the mean are constants there, and the two
+gradients have no derivative of their own.
 """
 from __future__ import annotations
 
 import ctypes
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib
 from ._lib import check
@@ -70,6 +77,63 @@ def _on(stream, call, *args):
         if isinstance(t, torch.Tensor):
             t.record_stream(stream)
     return result
+
+
+def _tracked(t: torch.Tensor) -> bool:
+    return t.requires_grad and torch.is_grad_enabled()
+
+
+def _written(out: torch.Tensor) -> None:
+    """Tells torch that a given `out` changed: a graph that needs its former values
+    refuses to go on without them."""
+    if not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+
+
+class _Lookup(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, rows, ids, scale):
+        ctx.save_for_backward(ids)
+        ctx.table = (table.shape[0], scale, table.dtype)
+        ctx.mark_dirty(rows)
+        return rows
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        ids, = ctx.saved_tensors
+        if ids.dim() == 0:
+            ids, grad = ids.unsqueeze(0), grad.unsqueeze(0)
+        return embed_lookup_grad(grad, ids, *ctx.table), None, None, None
+
+
+class _Pool(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, out, mean, mask):
+        ctx.save_for_backward(mean, mask)
+        ctx.dtype = hidden.dtype
+        ctx.mark_dirty(out)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        return embed_pool_grad(grad, *ctx.saved_tensors, ctx.dtype), None, None, None
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, loss, teacher_ids, teacher_scores, temperature):
+        ctx.save_for_backward(logits, teacher_ids, teacher_scores)
+        ctx.temperature = temperature
+        ctx.mark_dirty(loss)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        _, dlogits = distill_loss(*ctx.saved_tensors, ctx.temperature, grad)
+        return dlogits, None, None, None, None
 
 
 def _check_sizes(*sizes: int) -> None:
@@ -123,7 +187,8 @@ def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     _check_sizes(dim)
     device = _check_device(table, ids)
     shape = (*ids.shape, dim)
-    if out is None:
+    given = out is not None
+    if not given:
         out_dtype = out_dtype or table.dtype
         if out_dtype not in _DT:
             raise ValueError("out_dtype must be bfloat16 or float32")
@@ -140,7 +205,9 @@ def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     _call("oprag_embed_lookup",
           table.data_ptr(), _DT[table.dtype], vocab, dim, stride, ids.data_ptr(), _IDS[ids.dtype],
           ids.numel(), scale, out.data_ptr(), _DT[out.dtype], _stream(device))
-    return out
+    if given:
+        _written(out)
+    return _Lookup.apply(table, out, ids, scale) if _tracked(table) else out
 
 
 def embed_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0,
@@ -166,7 +233,8 @@ def embed_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: 
     device = _check_device(grad, ids)
     need = ctypes.c_int64()
     _call("oprag_embed_lookup_grad_workspace", count, vocab, dim, ctypes.byref(need))
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty((vocab, dim), dtype=out_dtype, device=device)
     elif (tuple(out.shape) != (vocab, dim) or out.dtype != out_dtype
           or not out.is_contiguous() or out.get_device() != device):
@@ -183,6 +251,8 @@ def embed_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: 
           grad.data_ptr(), _DT[grad.dtype], grad.shape[0], grad.shape[1], dim, *_strides(grad),
           ids.data_ptr(), _IDS[ids.dtype], vocab, scale, out.data_ptr(), _DT[out_dtype],
           None if work is None else work.data_ptr(), need.value, _stream(device))
+    if given:
+        _written(out)
     return out
 
 
@@ -214,7 +284,7 @@ def embed_pool_train(hidden: torch.Tensor, mask: torch.Tensor,
     _call("oprag_embed_pool_train",
           hidden.data_ptr(), _DT[hidden.dtype], b, t, d, mask.data_ptr(), out.data_ptr(),
           _DT[out_dtype], mean.data_ptr(), _stream(device))
-    return out, mean
+    return (_Pool.apply(hidden, out, mean, mask) if _tracked(hidden) else out), mean
 
 
 def embed_pool_grad(grad: torch.Tensor, mean: torch.Tensor, mask: torch.Tensor,
@@ -284,7 +354,7 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
         _check_device(logits, weight)
         weight = weight.contiguous()
     stride = out_stride = n
-    whole = logits.is_contiguous()
+    whole, given = logits.is_contiguous(), grad and out is not None
     if not grad:
         out = None
     elif out is None:
@@ -307,4 +377,8 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
           teacher_scores.data_ptr(), results[1], temperature,
           None if weight is None else weight.data_ptr(), loss.data_ptr(),
           None if out is None else out.data_ptr(), out_stride, _stream(device))
+    if _tracked(logits):
+        loss = _Distill.apply(logits, loss, teacher_ids, teacher_scores, temperature)
+    if given:                             # (behind the graph's note of the scores)
+        _written(out)
     return loss, out
