@@ -9,8 +9,8 @@ import torch
 from paper_2608_08340_gb300.train import (distill_loss, embed_lookup, embed_lookup_grad,
                                           embed_pool_grad, embed_pool_train)
 
-from test_gpu_train import (DT, _distill_plain, _pool_grad_plain, _rand, _tail_mask, _teacher,
-                            _within)
+from test_gpu_train import (DT, U, _check_distill, _distill_plain, _pool_grad_plain, _rand,
+                            _tail_mask, _teacher, _within, _zipf_ids)
 
 pytestmark = pytest.mark.gpu
 
@@ -135,3 +135,107 @@ def test_outputs_between_the_rows_of_the_inputs():
     assert torch.equal(embed_lookup_grad(grad[2:], ids[2:], 10, out=grad[:2].view(10, 32)), want)
     with pytest.raises(RuntimeError, match="overlap"):
         embed_lookup_grad(grad[1:], ids[1:], 10, out=grad[:2].view(10, 32))
+
+
+# ------------------------------------------------------- gradient of the lookup
+
+def _check_grad(grad, ids, vocab, scale, out):
+    """Against sums in 64 bits, formed on the GPU for some columns at a time; the bound
+    is that of test_gpu_train.py."""
+    got = embed_lookup_grad(grad, ids, vocab, scale, DT[out])
+    flat = ids.reshape(-1).long()
+    real = (flat >= 0) & (flat < vocab)
+    at = flat[real]
+    count = torch.bincount(at, minlength=vocab)[:, None]
+    for lo in range(0, grad.shape[-1], 256):
+        g = grad[..., lo:lo + 256].reshape(flat.numel(), -1)[real].double()
+        zero = torch.zeros(vocab, g.shape[1], dtype=torch.float64, device="cuda")
+        exact = torch.index_add(zero, 0, at, g) * scale
+        mag = torch.index_add(zero, 0, at, g.abs()) * abs(scale)
+        _within(got[:, lo:lo + 256], exact, (count + 1) * U * mag, out, f"columns from {lo}")
+
+
+def _check_whole_numbers(shape, dtype, ids, vocab):
+    """Sums of small whole numbers are exact in fp32 (below 2^24) in any order: no token is
+    lost, counted twice or added to another row."""
+    assert 3 * ids.numel() < 2 ** 24
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    grad = torch.randint(-3, 4, shape, generator=g, device="cuda").to(DT[dtype])
+    flat = ids.reshape(-1).long()
+    real = (flat >= 0) & (flat < vocab)
+    want = torch.zeros(vocab, shape[-1], dtype=torch.float64, device="cuda")
+    for lo in range(0, shape[-1], 256):
+        part = grad[..., lo:lo + 256].reshape(flat.numel(), -1)[real].double()
+        want[:, lo:lo + 256].index_add_(0, flat[real], part)
+    assert torch.equal(embed_lookup_grad(grad, ids, vocab).double(), want)
+
+
+# Row widths of every number of groups a lane, and of several column slabs; from 69632
+# tokens x slabs on, units of more than 16 items, up to 64 and 128.
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("vocab,dim,shape", [
+    (3000, 264, (50, 100)), (3000, 384, (50, 100)), (3000, 392, (50, 100)), (3000, 520, (50, 100)),
+    (3000, 768, (50, 100)), (3000, 776, (50, 100)), (3000, 1024, (7, 801)), (2000, 1032, (50, 100)),
+    (700, 4104, (60, 100)), (9, 2056, (5, 600)), (2000, 520, (100, 801)), (30522, 1032, (100, 400)),
+    (500, 768, (300, 999)), (50, 128, (40, 7001)), (500, 4104, (150, 401)), (3000, 8192, (90, 301))])
+def test_lookup_grad_of_wide_rows_and_large_units(dtype, out, vocab, dim, shape):
+    ids = _zipf_ids(shape, vocab, dim + vocab)
+    _check_grad(_rand((*shape, dim), dtype, dim), ids, vocab, 0.7, out)
+    _check_whole_numbers((*shape, dim), dtype, ids, vocab)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,tokens", [(768, 3000), (768, 300000), (1032, 100000), (4104, 70000)])
+def test_lookup_grad_of_a_few_long_rows(dtype, dim, tokens):
+    """Rows that cross many units, that end where a unit does, and single tokens beside them."""
+    ids = torch.full((tokens,), 40, device="cuda")
+    ids[tokens // 3:] = 41
+    ids[tokens // 2:] = 90
+    ids[::1000] = torch.arange(0, (tokens + 999) // 1000, device="cuda") % 97
+    grad = _rand((tokens, dim), dtype, dim)
+    _check_grad(grad, ids, 100, 1.0, "f32")
+    _check_whole_numbers((tokens, dim), dtype, ids, 100)
+    _check_grad(grad, torch.arange(tokens, device="cuda") // 256, tokens // 256 + 1, 1.0, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,texts,tokens", [(768, 1000, 300), (64, 1000, 300), (1032, 200, 250)])
+def test_lookup_grad_of_many_texts_that_share_a_gradient(dtype, dim, texts, tokens):
+    rows = _rand((texts, 1, dim), dtype, dim)
+    _check_grad(rows.expand(-1, tokens, -1), _zipf_ids((texts, tokens), 30522, 1), 30522, 3.0, "f32")
+
+
+# Tiles of 1024 tokens to 32768 of them, of 4096 beyond; more than 128 tiles beyond
+# 524288; one, two and three passes over the ids' digits.
+@pytest.mark.parametrize("bits", [torch.int32, torch.int64])
+@pytest.mark.parametrize("vocab", [5, 600, 2 ** 18, 2 ** 18 + 1, 1000003])
+@pytest.mark.parametrize("tokens", [2049, 32768, 32769, 44800, 131072, 131073, 524288, 524289, 1200001])
+def test_lookup_grad_of_sorts_of_every_size(bits, vocab, tokens):
+    if vocab < 2000:
+        ids = _zipf_ids((tokens,), vocab, tokens)
+    else:                                         # all of the digits
+        ids = torch.randint(-vocab // 8, vocab + vocab // 8, (tokens,), device="cuda",
+                            generator=torch.Generator(device="cuda").manual_seed(tokens))
+        ids[::3] = vocab - 1 - ids[::3] % 50
+    _check_grad(_rand((tokens, 8), "f32", vocab), ids.to(bits), vocab, 1.0, "f32")
+    _check_whole_numbers((tokens, 8), "bf16", ids.to(bits), vocab)
+
+
+# ------------------------------------------- distillation of more than 1 MB a row
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 600007), ("f32", 300011), ("bf16", 1048576)])
+@pytest.mark.parametrize("k", [129, 200, 256])
+def test_distill_of_many_results_in_large_rows(dtype, n, k):
+    q = 6
+    logits = _rand((q, n), dtype, n, 0.3)
+    ids, scores = _teacher(q, n, k, k)
+    ids[0, ::3] = ids[0, 1]                       # repeated ones
+    ids[1, k // 2:] = ids[1, :k - k // 2].clone()
+    logits[2, ids[2, :50]] = -math.inf            # hidden ones
+    logits[3, n // 4:n // 2] = torch.finfo(logits.dtype).min
+    ids[4, 7:] = -1                               # few
+    scores[5, k - 100:] = -math.inf
+    ids[5, 0], ids[5, 1] = n - 1, 0
+    weight = torch.linspace(-1, 2, q, device="cuda")
+    _, dz = _check_distill(logits, ids, scores, 0.2, weight)
+    assert (dz[2, ids[2, :50]] == 0).all() and (dz[3, n // 4:n // 2] == 0).all()
