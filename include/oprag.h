@@ -443,8 +443,10 @@ OPRAG_API int oprag_embed_lookup_grad_workspace(int64_t count, int64_t vocab, in
 /*
  * Gradient of the table: out[v] = scale * sum of grad[i] over the tokens i with
  * ids[i] = v, zeros for a row without tokens; ids outside [0, vocab) contribute
- * nothing.  Summed in fp32 in an order given by the ids: the same inputs give
- * the same bits.
+ * nothing (so that padding is best given as -1: the tokens of a padding id of the
+ * table are added up for its row, which makes that row the longest, and costs up
+ * to twice the time).  Summed in fp32 in an order given by the ids: the same inputs
+ * give the same bits.
  *   grad        device; token t of text b has dim values at b * text_stride +
  *               t * token_stride (in values; whole 16 bytes; 0 where tokens or
  *               texts share a gradient).
@@ -500,8 +502,15 @@ OPRAG_API int oprag_embed_pool_grad(const void *grad, int32_t grad_dtype, const 
  *   grad[i] = weight[i] / temperature * (p - t).
  * A result takes part if its id lies in [0, n), its score is above -inf and the
  * student's score of that chunk is above the lowest value of its dtype (that
- * value and -inf hide a chunk from the row).  An id that repeats adds its shares.  A row without such a
- * result has loss 0 and a zero gradient, a row of weight 0 a zero gradient.
+ * value and -inf hide a chunk from the row).  An id that repeats adds its shares.
+ * A row without such a result has loss 0 and a zero gradient, a row of weight 0 a
+ * zero gradient.
+ * Exponentials are the device's approximation of 2^x (2^-22 of their value), with
+ * 1 / temperature rounded into the exponent's factor: p and t are off by some
+ * (4 |x| + 4 mean |x| + 24) 2^-24 of themselves, x = (z - max z) / temperature; at
+ * 1024 x 32768 fp32 5e-7 of the results' size, where sums of expf are 3e-7 off.  The same call
+ * gives the same bits; a row's last bits may depend on how many rows the call
+ * has (few rows are split over more of the device).
  *   logits      device, q rows of n values, row_stride values apart; any
  *               alignment of the rows.
  *   teacher_ids, teacher_scores   device, q x k, k in [1, OPRAG_K_MAX].

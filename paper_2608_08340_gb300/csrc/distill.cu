@@ -14,10 +14,11 @@
 // the pairs (m, s), through distributed shared memory where a cluster has several CTAs,
 // gives the row's.  The gradient then goes backwards over the row: the last batches are
 // still in shared memory, the ones before come from L2, where the most recent are
-// likeliest to be.  256 rows of 2^20 bf16 scores: 229 us, 4.7 TB/s of the bytes that are
-// needed (DRAM reads 1.2 times the rows); 1024 x 32768 fp32 61 us; 300 x 50021 bf16 17 us.
-// About 90 instructions per group keep the issue slots half busy; barriers and first
-// loads of many small CTAs are the rest.
+// likeliest to be.  256 rows of 2^20 bf16 scores: 228 us, 4.7 TB/s of the bytes that are
+// needed (DRAM reads 1.2 times the rows), the loss alone 110; 1024 x 32768 fp32 60 us (38);
+// 300 x 50021 bf16 19 to 22 us (15): one wave that fills half of the places, whose CTAs all
+// read first and all write last.  About 90 instructions per group keep the issue slots half
+// busy; barriers and first loads of many small CTAs are the rest.
 //
 // Tried: rows kept whole in one CTA per SM (26 groups a thread), the next row's copies
 // flying meanwhile: 433 us for the first, 103 for the second line; persistent CTAs that
@@ -488,7 +489,7 @@ cudaError_t launch_rows(const DistillArgs& a, int ctas, cudaStream_t st) {
 // row; a row of more than 1 MB is split over 16 CTAs of 256 threads, four on an SM with
 // 48 KB each, so that the rows under way fit into L2 (some 50 MB hold).  Measured, us:
 // 2048 rows of 31 KB 128 threads 30, 256 threads 34; 300 of 98 KB in 1 / 2 / 4 CTAs 23 / 17 / 21;
-// 1024 of 128 KB 1 / 2 / 4 / 8 CTAs 71 / 61 / 59 / 70; 2000 of 195 KB 4 / 8 CTAs 149 / 166; 256 of
+// 1024 of 128 KB 1 / 2 / 4 / 8 CTAs 71 / 61 / 59 / 70 (the limit of 96 KB favours the former); 2000 of 195 KB 4 / 8 CTAs 149 / 166; 256 of
 // 586 KB 8 / 16 CTAs 72 / 77; 256 of 800 KB 4 / 8 / 16 CTAs 113 / 101 / 92; 256 of 2 MB 16 CTAs of 128
 // and 256 threads 236 and 229, 8 of 512 threads 241.  16 KB of a row in a CTA's shared
 // memory instead of 24: 195 KB rows 156, 800 KB rows 96.  Few rows are spread further, down

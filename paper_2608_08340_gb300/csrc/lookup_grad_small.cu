@@ -8,7 +8,8 @@
 //
 // Bound by the table's bytes and one launch: 256 tokens into 30522 x 768 fp32 rows (94 MB,
 // 13.9 us of HBM) 24 us.  One CTA adds up a row, however many tokens it has: 1024 of one row
-// of 768 columns take 103 us, which is one reason for the limit (few_tokens).
+// of 768 columns take 103 us, which is one reason for the limit (few_tokens), and 16 texts of
+// 64 tokens padded with one id of the table 72 us, with -1 36.
 #include "lookup_grad.cuh"
 #include "values.cuh"
 

@@ -215,7 +215,9 @@ def embed_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: 
                       out=None) -> torch.Tensor:
     """Gradient of embed_lookup for its table: (vocab, dim) in out_dtype, row v
     scale times the sum of grad over the tokens whose id is v (float32 sums in an
-    order given by the ids; zeros for a row without tokens).
+    order given by the ids; zeros for a row without tokens).  Padding is best given
+    as -1 (ids.masked_fill(ids == pad, -1)): the tokens of a padding id of the table are
+    added up like any other's, in up to twice the time.
 
     grad: ids.shape + (dim,) bfloat16 or float32; it may be a broadcast, such as
     rows.unsqueeze(1).expand(-1, tokens, -1) where all tokens of a text share a row:
@@ -335,7 +337,11 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
 
     weight: (q,) float32, default 1 for every row.  A row without results has loss 0
     and no gradient.  grad=False: (loss, None).  out: where the gradient goes, a (q, n)
-    tensor with contiguous rows; it may be logits."""
+    tensor with contiguous rows; it may be logits, or lie apart from its rows.
+
+    p and t carry the device's approximate exponential: some (4 |x| + 4 mean |x| + 24) 2^-24
+    of themselves for x = (logits - max) / temperature, up to twice what expf leaves.  The
+    same call gives the same bits; a row's last bits may depend on q."""
     if stream is not None:
         return _on(stream, distill_loss, logits, teacher_ids, teacher_scores, temperature, weight,
                    grad, None, out)
